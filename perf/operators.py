@@ -415,9 +415,11 @@ def run(st):
     if not own:
         return {"norm": _norm_plain, "append": _append_plain, "attend": _attend_plain}[c["kind"]](st)
     if c["kind"] == "norm":
-        _, scales, values = _ctx().rmsnorm_quant(
+        codes, scales, values = _ctx().rmsnorm_quant(
             st["x"], residual=st["residual"], residual_out=st["sum"], gain=st["gain"], eps=1e-6, bits=c["bits"],
-            clip=c["clip"], codes=st["codes"], scales=st["scales"], values=st["values"])
+            clip=c["clip"], codes=st["codes"], scales=st["scales"], values=None if c["out"] == "codes" else st["values"])
+        if c["out"] == "codes":  # what the codes stand for
+            values = torch.mul(codes, scales[:, None], out=st["values"])
         return {"values": values, "scales": scales, "sum": st["sum"]}
     if c["kind"] == "append":
         _ctx().kv_append(st["cache"], st["batch"], st["q"], st["k"], st["v"], rope=st["rope"], hadamard=c["hadamard"],
