@@ -840,8 +840,8 @@ __global__ void __launch_bounds__(256) k_kv_attend_join_runs(const AttendParams 
       for (int w = 0; w < 8; ++w) {
         const float t = ranges[w][HD], l = ranges[w][HD + 1];
         const float f = t == -INFINITY && l == 0.f ? 0.f : exp2_fast(t - most);
+        sum = fmaf(f, l, sum);  // (the factor 0 too: a range may hold NaN only, or far below the others)
         if (f == 0.f) continue;
-        sum = fmaf(f, l, sum);
 #pragma unroll
         for (int e = 0; e < HD / 32; ++e) acc[e] = fmaf(f, ranges[w][lane * (HD / 32) + e], acc[e]);
       }
