@@ -550,8 +550,8 @@ kt_status kt_kv_append(kt_ctx* ctx, const kt_kv_cache* cache, const kt_kv_batch*
  * scale in 0..1e30 (KT_ERR_INVALID_ARG otherwise).
  * A row that sees no token gets zeros and lse -inf.  Tokens that a row does not
  * see never touch it, whatever they hold; a row that sees a token whose scale or
- * shift is no number gets NaN (a prompt's row: its lse too).  out may be Q's own matrix.  `scratch` (device, 256-byte aligned, not the
- * context's workspace) holds kt_kv_scratch_bytes() bytes for this cache, batch
+ * shift is NaN, or whose value's is an infinity, gets NaN, out and lse.  out may be
+ * Q's own matrix.  `scratch` (device, 256-byte aligned, not the context's workspace) holds kt_kv_scratch_bytes() bytes for this cache, batch
  * and head count; its contents matter only during the call, and two calls that
  * may overlap need two.  A sequence whose rows or length are out of their bounds
  * is skipped, its rows left as they were; rows of a sequence with a page id out

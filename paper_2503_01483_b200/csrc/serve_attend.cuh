@@ -689,6 +689,9 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 2) k_kv_attend_rows(
         ll += __shfl_xor_sync(0xffffffffu, ll, x);
         bb += __shfl_xor_sync(0xffffffffu, bb, x);
       }
+      // A value that is no number makes the row's sum NaN, which every join keeps: its output would be lost where this part
+      // lies so far below the row's maximum that its factor is 0.
+      if (!(fabsf(bb) < __uint_as_float(0x7f800000u))) ll = __uint_as_float(0x7fc00000u);
       float* dst = join + (warp * NR + nt * 8 + 2 * c + i) * kRow;
       const float g_down = power_of_two(exponent(big[nt][i]) - 2);
 #pragma unroll

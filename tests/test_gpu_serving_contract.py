@@ -47,7 +47,7 @@ def token_sets(n):
 
 @pytest.mark.parametrize("layout", list(LAYOUTS))
 @pytest.mark.parametrize("tokens", ["newest", "last tiles", "first tiles", "inside"])
-@pytest.mark.parametrize("name,kind", [("k", "scale"), ("k", "shift")])
+@pytest.mark.parametrize("name,kind", [("k", "scale"), ("k", "shift"), ("v", "scale"), ("v", "shift"), ("v", "inf")])
 @pytest.mark.parametrize("far", [False, True])
 def test_a_row_that_sees_what_is_no_number_gets_nan(ctx, layout, tokens, name, kind, far):  # noqa: F811
     n = LAYOUTS[layout][1][0]
