@@ -310,7 +310,7 @@ static kt_status plan_attend(int sm_count, const kt_kv_cache& c, const kt_kv_bat
   pl->nt = pl->prompt ? 32 : packed <= 8 ? 1 : 2;
   const int nr = 8 * pl->nt;
   const long long row_blocks = (packed + nr - 1) / nr;
-  if (row_blocks > 0x7fffffffll) return KT_ERR_SHAPE;
+  if (row_blocks * nr > 0x7fffffffll) return KT_ERR_SHAPE;  // (a block's first packed row is a 32-bit number)
   pl->row_blocks = static_cast<int>(row_blocks);
   pl->seqs = b.n_seqs;
   if (pl->prompt) {

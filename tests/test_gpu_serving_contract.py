@@ -65,3 +65,17 @@ def test_a_row_that_sees_what_is_no_number_gets_nan(ctx, layout, tokens, name, k
         assert bool(out[r, :group].isnan().all() if nan else out[r, :group].isfinite().all()), r
         assert bool(lse[r, :group].isnan().all() if nan else lse[r, :group].isfinite().all()), r
         assert bool(out[r, group:].isfinite().all()) and bool(lse[r, group:].isfinite().all())   # the other key head
+
+
+# ------------------------------------------------------------------------------------------------- host bounds
+@pytest.mark.parametrize("max_rows,group,fits", [(2**28, 16, False), (2**30, 2, False), (2**30, 64, False), (2**27, 16, False),
+                                                 (2**30, 1, True), (2**27, 15, True)])
+def test_rows_of_a_key_head_are_counted_in_32_bits(ctx, max_rows, group, fits):  # noqa: F811
+    sq = Seqs([1], [30], 16)
+    cache = kurtail.KvCache.empty(sq.pages, 1, 16, 64, 4, DEV)
+    if fits:
+        assert sq.batch(ctx, cache, group, max_rows=max_rows).max_rows == max_rows   # (nothing is launched)
+        return
+    with pytest.raises(kurtail.KtError) as e:
+        sq.batch(ctx, cache, group, max_rows=max_rows)
+    assert e.value.status == 2
