@@ -508,8 +508,9 @@ typedef struct {
  * lengths[s] - rows .. lengths[s] - 1 (lengths[s] counts them).  Its token j lies
  * in page page_table[s][j / page_size].  The arrays are on the device and may
  * change between calls (and between replays of a graph) within the two host
- * bounds, which size the launches.  Rows behind row_starts[n_seqs] (padding) are
- * neither read nor written.  A sequence may have no rows or no tokens. */
+ * bounds, which size the launches.  Rows behind row_starts[n_seqs] (padding), or
+ * in front of row_starts[0], are neither used nor written.  A sequence may have no
+ * rows or no tokens. */
 typedef struct {
   const int32_t* row_starts; /* [n_seqs + 1], ascending */
   const int32_t* lengths;    /* [n_seqs] */
@@ -535,8 +536,11 @@ typedef struct {
  * may be Q's own matrix).  K_values, V_values (KT_BF16, NULL: not wanted) receive
  * what the cache now stands for: the simulated quantisation of the paper's own
  * evaluation.  A head that holds a NaN or an infinity gets scale and shift NaN
- * and codes 0.  A row whose position, length or page is out of bounds is
- * skipped.  Two rows must not name the same token of the cache.  Matrices need
+ * and codes 0.  A row whose position, length or page is out of bounds is skipped,
+ * and so are all rows of a sequence whose starts do not fit the matrices or
+ * max_rows.  A sequence shorter than its rows is such an error here (its first rows
+ * have no position), while kt_kv_attend takes these as rows that see nothing.
+ * Two rows must not name the same token of the cache.  Matrices need
  * 16-byte aligned bases and leading dimensions (KT_ERR_ALIGN). */
 kt_status kt_kv_append(kt_ctx* ctx, const kt_kv_cache* cache, const kt_kv_batch* batch, const kt_mat* Q, kt_mat K,
                        kt_mat V, const float* rope, int64_t rope_rows, int32_t hadamard, const kt_quant_spec* spec,

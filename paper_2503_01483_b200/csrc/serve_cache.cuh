@@ -44,9 +44,9 @@ struct AppendParams {
 constexpr unsigned int kCacheErrBatch = 1;  // row_starts, lengths or positions out of their bounds
 constexpr unsigned int kCacheErrPage = 2;   // a page id out of range
 
-// The sequence s with row_starts[s] <= row < row_starts[s + 1], found by the whole warp in steps of 32; -1 if there is
-// none (rows behind the last sequence, or starts that do not ascend).
-__device__ __forceinline__ int find_sequence(const int* row_starts, int n_seqs, int row) {
+// The sequence s with row_starts[s] = begin <= row < end = row_starts[s + 1], found by the whole warp in steps of 32; -1 if
+// there is none (rows in front of the first sequence or behind the last, or starts that do not ascend).
+__device__ __forceinline__ int find_sequence(const int* row_starts, int n_seqs, int row, int* begin, int* end) {
   const int lane = threadIdx.x & 31;
   int lo = 0, n = n_seqs;  // the candidates are lo .. lo + n - 1
   while (n > 1) {
@@ -57,8 +57,9 @@ __device__ __forceinline__ int find_sequence(const int* row_starts, int n_seqs, 
     lo += part * step;
     n = min(step, n - part * step);
   }
-  if (plain_load(row_starts + lo) <= row && row < plain_load(row_starts + lo + 1)) return lo;
-  return -1;
+  *begin = plain_load(row_starts + lo);
+  *end = plain_load(row_starts + lo + 1);
+  return *begin <= row && row < *end ? lo : -1;
 }
 
 // Two float32 operations in one instruction; each half is rounded like the single operation.
@@ -326,12 +327,14 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 4 ? 6 : 2) k_kv_append(co
     w.pos = -1;
     w.at = 0;
     float4 turn = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int s = find_sequence(p.b.row_starts, p.b.n_seqs, row);
+    int begin, end;
+    const int s = find_sequence(p.b.row_starts, p.b.n_seqs, row, &begin, &end);
+    unsigned int wrong = 0u;
     if (s >= 0) {
       const int length = plain_load(p.b.lengths + s);
-      const int pos = max(length, 0) - (plain_load(p.b.row_starts + s + 1) - row);
-      unsigned int wrong = 0u;
-      if (length < 0 || pos < 0 || length > p.b.max_length ||
+      const int pos = max(length, 0) - (end - row);
+      // (a sequence whose rows do not fit is skipped whole, as the attention does: its rows' positions cannot be told)
+      if (begin < 0 || end > p.rows || end - begin > p.b.max_rows || length < 0 || pos < 0 || length > p.b.max_length ||
           static_cast<long long>(length) > (static_cast<long long>(p.b.table_ld) << p.c.page_shift) ||
           (p.rope != nullptr && pos >= p.rope_rows)) {
         wrong = kCacheErrBatch;
@@ -347,8 +350,10 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 4 ? 6 : 2) k_kv_append(co
           w.at = (static_cast<long long>(page) * H << p.c.page_shift) + (pos & ((1 << p.c.page_shift) - 1));
         }
       }
-      if (wrong != 0u && lane == 0) atomicMax(p.err, wrong);
+    } else if (row >= plain_load(p.b.row_starts) && row < plain_load(p.b.row_starts + p.b.n_seqs)) {
+      wrong = kCacheErrBatch;  // starts that do not ascend
     }
+    if (wrong != 0u && lane == 0) atomicMax(p.err, wrong);
     if (lane == 0) place[t] = w;
     if (lane < LPH * 4) turns[t][lane / 4 * 5 + lane % 4] = make_float4(turn.x, turn.z, turn.y, turn.w);
   }

@@ -79,3 +79,68 @@ def test_rows_of_a_key_head_are_counted_in_32_bits(ctx, max_rows, group, fits): 
     with pytest.raises(kurtail.KtError) as e:
         sq.batch(ctx, cache, group, max_rows=max_rows)
     assert e.value.status == 2
+
+
+# ------------------------------------------------------------------------------------------------- row starts of an append
+def test_append_skips_sequences_whose_rows_do_not_fit_and_says_so(ctx):  # noqa: F811
+    # long sequences, so that a row that is taken for another one still has a position of the sequence
+    hd, page, length = 64, 16, 300
+    k = rand(1, 9, hd).to(BF16).to(DEV)
+    q = rand(2, 9, 2 * hd).to(BF16).to(DEV)
+    for starts, max_rows, skipped in (([0, 3, 6, 10], 5, [2]),        # past the matrices
+                                      ([0, 3, 6, 9], 2, [0, 1, 2]),   # more rows than the bound
+                                      ([0, 5, 7, 9], 4, [0]),
+                                      ([-2, 3, 6, 9], 5, [0])):
+        sq = Seqs([3, 3, 3], [length] * 3, page)
+        cache = kurtail.KvCache.empty(sq.pages, 1, page, hd, 8, DEV)
+        batch = sq.batch(ctx, cache, 2, max_rows=max_rows)
+        batch.row_starts.copy_(torch.tensor(starts, dtype=torch.int32))
+        out = torch.full_like(q, 55.0)
+        ctx.kv_append(cache, batch, q, k, k, q_out=out)
+        with pytest.raises(kurtail.KtError) as e:
+            ctx.check()
+        assert e.value.status == 12, starts
+        left = torch.ones(9, dtype=torch.bool)
+        for s in range(3):
+            a, b = starts[s], starts[s + 1]
+            written = [bool(cache.k_codes[p, 0, o].any()) for p, o in (sq.at(s, j) for j in range(length))]
+            if s in skipped:
+                assert not any(written), (starts, s)
+            else:
+                assert written == [False] * (length - b + a) + [True] * (b - a), (starts, s)
+                left[a:b] = False
+        assert bool((out.cpu()[left] == 55.0).all()) and bool((out.cpu()[~left] != 55.0).any(1).all()), starts
+
+
+def test_append_says_so_where_starts_do_not_ascend(ctx):  # noqa: F811
+    hd, page = 64, 16
+    sq = Seqs([3, 3, 3], [300] * 3, page)
+    cache = kurtail.KvCache.empty(sq.pages, 1, page, hd, 8, DEV)
+    k = rand(1, 9, hd).to(BF16).to(DEV)
+    for starts in ([0, 6, 3, 9], [0, 4, 2, 4]):   # (rows between two such starts have no owner, or two)
+        batch = sq.batch(ctx, cache, 1, max_rows=9)
+        batch.row_starts.copy_(torch.tensor(starts, dtype=torch.int32))
+        ctx.kv_append(cache, batch, None, k, k)
+        with pytest.raises(kurtail.KtError) as e:
+            ctx.check()
+        assert e.value.status == 12, starts
+
+
+def test_rows_in_front_of_the_first_sequence_belong_to_none(ctx):  # noqa: F811
+    hd, page = 64, 16
+    sq = Seqs([2, 1], [40, 33], page)
+    k, q = rand(1, 6, hd).to(BF16).to(DEV), rand(2, 6, 2 * hd).to(BF16).to(DEV)
+    got = []
+    for front in (0, 2):
+        cache = kurtail.KvCache.empty(sq.pages, 1, page, hd, 8, DEV)
+        batch = sq.batch(ctx, cache, 2)
+        batch.row_starts.add_(front)
+        out = torch.full_like(q, 55.0)
+        shift = lambda t: t.roll(front, 0)  # noqa: E731
+        ctx.kv_append(cache, batch, shift(q), shift(k), shift(k), q_out=out)
+        ctx.kv_attend(cache, batch, out, out=out)
+        ctx.check()
+        assert bool((out[:front] == 55.0).all()) and bool((out[front + 3 :] == 55.0).all())
+        got.append((out[front : front + 3].clone(), cache.k_codes))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
