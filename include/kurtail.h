@@ -516,7 +516,7 @@ typedef struct {
   const int32_t* lengths;    /* [n_seqs] */
   const int32_t* page_table; /* [n_seqs][table_ld] */
   int32_t n_seqs;
-  int32_t table_ld;
+  int32_t table_ld;          /* columns: page ids are followed up to this one */
   int32_t max_rows;          /* no sequence has more rows (2^30 at most; attention: times the
                                 query heads of a key head, 2^31 - 256 at most) */
   int32_t max_length;        /* no sequence has more tokens (2^30 at most) */

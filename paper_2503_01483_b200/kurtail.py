@@ -238,7 +238,7 @@ class KvBatch:
     """The sequences of a call (kt_kv_batch) and the scratch of their attention; made by Context.kv_batch().
 
     The three index tensors may be rewritten in place between calls and between replays of a captured graph, within
-    max_rows and max_length.  Two calls that may overlap need two KvBatch objects (each owns one scratch buffer).
+    max_rows and max_length (lowered to what page_table's own columns hold, where it is columns of a wider table).  Two calls that may overlap need two KvBatch objects (each owns one scratch buffer).
     """
 
     def __init__(self, row_starts, lengths, page_table, max_rows, max_length):
@@ -258,6 +258,21 @@ class KvBatch:
                               self.max_rows, self.max_length)
         self._ref, self._at = C.byref(self._c), C.addressof(self._c)
         self.q_heads, self.scratch, self._scratch_ptr, self._scratch_bytes = 0, None, 0, 0
+        self._page_size = 0 if ld > page_table.shape[1] else None   # of a table that is columns of a wider one
+
+    def _own_columns(self, cache):
+        """The kernels know a table's pitch and take it for its width: of a table that is columns of a wider one, its own
+        columns bound the lengths, for caches of this page size."""
+        if self._page_size is not None:
+            self._page_size = cache.page_size
+            self._c.max_length = self.max_length = min(self.max_length, self.page_table.shape[1] * cache.page_size)
+
+    def _fits(self, cache, index):
+        if self.index != index or cache.index != index:
+            raise ValueError("cache and batch must be on the context's device")
+        if self._page_size is not None and self._page_size != cache.page_size:
+            raise ValueError("a page table that is columns of a wider one needs the batch of Context.kv_batch, and caches of "
+                             "that call's page size")
 
 
 class Context:
@@ -514,7 +529,8 @@ class Context:
         """A KvBatch with the scratch that kv_attend needs for this cache and head count (make it before capturing a graph
         that uses it)."""
         batch = KvBatch(row_starts, lengths, page_table, max_rows, max_length)
-        _need(batch.index == self._index and cache.index == self._index, "cache and indices must be on the context's device")
+        batch._own_columns(cache)
+        batch._fits(cache, self._index)
         n = C.c_size_t()
         _check(lib().kt_kv_scratch_bytes(self._h, cache._ref, batch._ref, q_heads, C.byref(n)), "kt_kv_scratch_bytes")
         batch.q_heads = q_heads
@@ -528,8 +544,7 @@ class Context:
                   k_values=None, v_values=None):
         """kt_kv_append.  q (None: keys and values only), k, v: rows x heads*head_dim, bf16 or f32.  Returns q_out, the
         turned queries in bf16 (allocated if not given; may be q itself)."""
-        if batch.index != self._index or cache.index != self._index:
-            raise ValueError("cache and batch must be on the context's device")
+        batch._fits(cache, self._index)
         if q is not None and q_out is None:
             q_out = self._new(q.shape, torch.bfloat16)
         st = _serving.kv_append(self._at, self._index, cache._at, batch._at, q, k, v, rope, hadamard, asymmetric, clip,
@@ -542,8 +557,7 @@ class Context:
         """kt_kv_attend.  q: rows x q_heads*head_dim bf16; scale: 1/sqrt(head_dim) if not given; lse: float32
         rows x q_heads to be filled, or None.  Returns out (allocated if not given: rows that no sequence owns, or of a
         sequence out of bounds, are then whatever the memory held)."""
-        if batch.index != self._index or cache.index != self._index:
-            raise ValueError("cache and batch must be on the context's device")
+        batch._fits(cache, self._index)
         if out is None:
             out = self._new(q.shape, torch.bfloat16)
         st = _serving.kv_attend(self._at, self._index, cache._at, batch._at, q, out, lse,

@@ -144,3 +144,38 @@ def test_rows_in_front_of_the_first_sequence_belong_to_none(ctx):  # noqa: F811
         got.append((out[front : front + 3].clone(), cache.k_codes))
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------------------------- page tables
+@pytest.mark.parametrize("rows,group", [([2, 1], 4), ([70, 9], 4)])
+def test_lengths_past_a_tables_own_columns_are_skipped(ctx, rows, group):  # noqa: F811
+    hd, page = 64, 16
+    sq = Seqs(rows, [90, 40], page)
+    cache, _, _ = filled_cache(sq, 1, hd, 8, seed=8, garbage=False)
+    q = rand(2, sq.N, group * hd).to(BF16).to(DEV)
+    k = rand(3, sq.N, hd).to(BF16).to(DEV)
+    batch = sq.batch(ctx, cache, group, max_length=1000)
+    want = ctx.kv_attend(cache, batch, q).clone()
+    n = sq.table.shape[1]
+    wide = torch.zeros(2, n + 7, dtype=torch.int32, device=DEV)      # ids that a cache has, around the table
+    wide[:, 5 : 5 + n] = batch.page_table
+    part = ctx.kv_batch(cache, group, batch.row_starts, batch.lengths, wide[:, 5 : 5 + n], max(rows), 1000)
+    assert torch.equal(ctx.kv_attend(cache, part, q), want)
+    ctx.check()
+    part.lengths[1] = n * page + 1                                    # one token behind the last row's own columns
+    out = torch.full_like(q, 55.0)
+    ctx.kv_attend(cache, part, q, out=out)
+    with pytest.raises(kurtail.KtError) as e:
+        ctx.check()
+    assert e.value.status == 12
+    assert torch.equal(out[: rows[0]], want[: rows[0]]) and bool((out[rows[0] :] == 55.0).all())
+    qo = torch.full_like(q, 55.0)
+    ctx.kv_append(cache, part, q, k, k, q_out=qo)
+    with pytest.raises(kurtail.KtError) as e:
+        ctx.check()
+    assert e.value.status == 12
+    assert bool((qo[: rows[0]] != 55.0).any(1).all()) and bool((qo[rows[0] :] == 55.0).all())
+    other = kurtail.KvCache.empty(30, 1, 32, hd, 8, DEV)
+    for call in (lambda: ctx.kv_attend(other, part, q), lambda: ctx.kv_append(other, part, q, k, k)):
+        with pytest.raises(ValueError):
+            call()

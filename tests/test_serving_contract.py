@@ -1,0 +1,41 @@
+"""Host-side promises of the serving calls' Python side that need no GPU."""
+import pytest
+import torch
+
+from paper_2503_01483_b200 import kurtail
+
+
+def ints(*a):
+    return torch.zeros(*a, dtype=torch.int32)
+
+
+def a_cache(page=16):
+    return kurtail.KvCache(*[torch.zeros(3, 2, page, 64, dtype=torch.uint8)] * 2, *[torch.zeros(3, 2, page, 2)] * 2, 8)
+
+
+def test_a_table_of_a_wider_ones_columns_bounds_the_lengths_by_its_own():
+    # the library is told the pitch of its rows and would follow page ids behind them, past the last row's end
+    wide = ints(2, 10)
+    for table, page, want in ((wide[:, 4:], 16, 96), (wide[:, :5], 16, 80), (wide[:, 4:], 64, 100), (wide, 16, 100),
+                              (wide[:1, 4:], 16, 100)):
+        b = kurtail.KvBatch(ints(table.shape[0] + 1), ints(table.shape[0]), table, 1, 100)
+        b._own_columns(a_cache(page))
+        assert b._c.max_length == b.max_length == want
+        assert b._c.max_length <= table.shape[1] * page or b._c.table_ld == table.shape[1]
+        b._fits(a_cache(page), -1)
+
+
+def test_such_a_table_is_for_one_page_size():
+    b = kurtail.KvBatch(ints(3), ints(2), ints(2, 10)[:, 4:], 1, 100)
+    for cache in (a_cache(16), a_cache(64)):
+        with pytest.raises(ValueError):
+            b._fits(cache, -1)
+    b._own_columns(a_cache(16))
+    b._fits(a_cache(16), -1)
+    with pytest.raises(ValueError):
+        b._fits(a_cache(32), -1)
+    with pytest.raises(ValueError):
+        b._fits(a_cache(16), 0)
+    whole = kurtail.KvBatch(ints(3), ints(2), ints(2, 10), 1, 100)
+    whole._own_columns(a_cache(16))
+    whole._fits(a_cache(64), -1)
