@@ -251,9 +251,10 @@ class KvBatch:
               and page_table.stride(1) == 1, "page_table must be [sequences, pages]")
         self.row_starts, self.lengths, self.page_table = row_starts, lengths, page_table
         self.max_rows, self.max_length = int(max_rows), int(max_length)
+        _need(abs(self.max_rows) < 2**31 and abs(self.max_length) < 2**31, "max_rows and max_length must fit 32 bits")
         self.index = row_starts.get_device()
         ld = page_table.stride(0) if page_table.shape[0] > 1 else page_table.shape[1]
-        _need(ld >= page_table.shape[1] and page_table.shape[1] < 2**31, "page_table rows overlap")
+        _need(page_table.shape[1] <= ld < 2**31, "page_table rows overlap, or lie 2^31 entries apart")
         self._c = kt_kv_batch(row_starts.data_ptr(), lengths.data_ptr(), page_table.data_ptr(), lengths.numel(), ld,
                               self.max_rows, self.max_length)
         self._ref, self._at = C.byref(self._c), C.addressof(self._c)

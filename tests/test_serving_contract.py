@@ -39,3 +39,12 @@ def test_such_a_table_is_for_one_page_size():
     whole = kurtail.KvBatch(ints(3), ints(2), ints(2, 10), 1, 100)
     whole._own_columns(a_cache(16))
     whole._fits(a_cache(64), -1)
+
+
+def test_bounds_that_do_not_fit_32_bits_are_refused():
+    # (a ctypes field takes such a number modulo 2^32)
+    make = lambda rows=1, length=10, table=ints(2, 5): kurtail.KvBatch(ints(3), ints(2), table, rows, length)  # noqa: E731
+    assert make(2**30, 2**30)._c.max_length == 2**30
+    for bad in (dict(rows=2**32 + 1), dict(length=2**32 + 10), dict(rows=2**31), dict(length=-(2**31) - 5)):
+        with pytest.raises(ValueError):
+            make(**bad)
