@@ -55,10 +55,11 @@ const at::Tensor& tensor(PyObject* o, const char* what) {
   if (!THPVariable_Check(o)) refuse("%s must be a tensor", what);
   return THPVariable_Unpack(o);
 }
-// A row-major matrix on the context's device.
+// A row-major matrix on the context's device.  (A stride along a dimension of one entry says nothing: a transposed column is
+// a row as good as any.)
 kt_mat matrix(PyObject* o, int device, const char* what) {
   const at::Tensor& t = tensor(o, what);
-  if (t.dim() != 2 || t.stride(1) != 1 || t.get_device() != device)
+  if (t.dim() != 2 || (t.stride(1) != 1 && t.size(1) != 1) || t.get_device() != device)
     refuse("%s must be 2-D with unit column stride, on the context's device", what);
   kt_mat m = {};
   if (t.scalar_type() == at::kBFloat16) m.dtype = KT_BF16;
@@ -67,7 +68,7 @@ kt_mat matrix(PyObject* o, int device, const char* what) {
   m.data = t.data_ptr();
   m.rows = t.size(0);
   m.cols = t.size(1);
-  m.ld = t.stride(0);
+  m.ld = m.rows == 1 ? m.cols : t.stride(0);
   return m;
 }
 struct MatrixOrNone {

@@ -179,3 +179,23 @@ def test_lengths_past_a_tables_own_columns_are_skipped(ctx, rows, group):  # noq
     for call in (lambda: ctx.kv_attend(other, part, q), lambda: ctx.kv_append(other, part, q, k, k)):
         with pytest.raises(ValueError):
             call()
+
+
+# ------------------------------------------------------------------------------------------------- single rows
+def test_a_row_is_one_whatever_its_stride(ctx):  # noqa: F811
+    hd = 64
+    x = rand(1, 4 * hd, 1).to(BF16).to(DEV).t()                          # one row, contiguous, of stride 1
+    assert x.stride(0) == 1
+    c, s, v = ctx.rmsnorm_quant(x, residual=x, bits=8, values=torch.empty_like(x), codes=torch.empty(1, 4 * hd, dtype=torch.int8, device=DEV))
+    wc, ws, wv = ctx.rmsnorm_quant(x.clone(memory_format=torch.contiguous_format).view(1, -1), residual=x.reshape(-1)[None], bits=8,
+                                   values=torch.empty(1, 4 * hd, dtype=BF16, device=DEV),
+                                   codes=torch.empty(1, 4 * hd, dtype=torch.int8, device=DEV))
+    assert torch.equal(c, wc) and torch.equal(s, ws) and torch.equal(v, wv)
+    sq = Seqs([1], [40], 16)
+    caches = [kurtail.KvCache.empty(sq.pages, 1, 16, hd, 8, DEV) for _ in range(2)]
+    outs = []
+    for cache, q in zip(caches, (x, x.reshape(-1)[None])):
+        batch = sq.batch(ctx, cache, 4)
+        outs.append(ctx.kv_attend(cache, batch, ctx.kv_append(cache, batch, q, q[:, :hd], q[:, hd : 2 * hd])))
+    ctx.check()
+    assert torch.equal(*outs) and torch.equal(caches[0].k_codes, caches[1].k_codes)

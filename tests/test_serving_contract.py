@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2503_01483_b200 import kurtail
+from paper_2503_01483_b200 import build, kurtail
 
 
 def ints(*a):
@@ -48,3 +48,16 @@ def test_bounds_that_do_not_fit_32_bits_are_refused():
     for bad in (dict(rows=2**32 + 1), dict(length=2**32 + 10), dict(rows=2**31), dict(length=-(2**31) - 5)):
         with pytest.raises(ValueError):
             make(**bad)
+
+
+def test_strides_of_single_columns_and_rows_say_nothing():
+    build.build()
+    kurtail.lib()
+    from paper_2503_01483_b200 import _serving
+    call = lambda x: _serving.rmsnorm_quant(0, -1, x, None, None, None, 1e-6, None, 1.0, None, None, x)  # noqa: E731
+    x = torch.zeros(8, 8)
+    for t in (x[:1].t(), x[:, 2:3], torch.zeros(8, 1).t()):                  # (no context: status 1, behind all checks of tensors)
+        assert call(t) == 1
+    for t in (x[:2].t(), x[:, ::2], x[:, :1].t()):
+        with pytest.raises(ValueError):
+            call(t)
