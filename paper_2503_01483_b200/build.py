@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import sys
 import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -32,8 +33,22 @@ def _older(out, sources):
     return any(os.path.getmtime(p) > t for p in deps)
 
 
+def built_for():
+    """The Python and the torch that _serving.so is built against; a module that names others is not used."""
+    import torch
+    return f"Python {sys.version.split()[0]}, torch {torch.__version__}"
+
+
+def _serving_stale():
+    """_serving.so is missing, older than its sources, or built against another Python or torch."""
+    if _older(SERVING, ["binding.cpp"]):
+        return True
+    with open(SERVING, "rb") as f:
+        return built_for().encode() + b"\0" not in f.read()
+
+
 def needs_build():
-    return _older(LIB, SOURCES + HEADERS) or _older(SERVING, ["binding.cpp"])
+    return _older(LIB, SOURCES + HEADERS) or _serving_stale()
 
 
 def _run(cmd, verbose):
@@ -50,11 +65,11 @@ def build(force=False, verbose=False):
         _run([_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-t", str(len(SOURCES)), "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v" if verbose else "-warn-spills",
               "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES], verbose)
-    if force or _older(SERVING, ["binding.cpp"]):
+    if force or _serving_stale():
         import torch
         root = os.path.dirname(torch.__file__)
         _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall",
-              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DKT_BUILT_FOR="{built_for()}"',
               "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(root, "include"),
               "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
               "-o", SERVING, os.path.join(CSRC, "binding.cpp"), "-L" + os.path.join(root, "lib"),

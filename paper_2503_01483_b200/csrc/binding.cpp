@@ -1,6 +1,7 @@
 // The serving calls from Python: tensors are described, checked and handed to libkurtail.so here.  A single token's call
 // takes the GPU 3 to 11 us; reading six tensors and filling the structures took 5 us in Python, 0.6 us here.  The library's
-// entry points are given as addresses (bind), so this module is not linked with it.
+// entry points are given as addresses (bind), so this module is not linked with it.  KT_BUILT_FOR names the Python and the
+// torch whose headers it was built with.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -113,9 +114,16 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+template <typename F>
+F bound(F f) {
+  if (f == nullptr) refuse("the library is not loaded (kurtail.lib() binds its entry points)");
+  return f;
+}
+
 // ctx, device, x, residual, residual_out, gain, eps, bits, clip, codes, scales, values -> status
 PyObject* rmsnorm_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded<12>(n, [&] {
+    const auto call = bound(g_rmsnorm_quant);
     const int dev = integer32(a[1], "device");
     const kt_mat x = matrix(a[2], dev, "x");
     const MatrixOrNone residual(a[3], dev, "residual"), sum(a[4], dev, "residual_out"), values(a[11], dev, "values");
@@ -131,8 +139,7 @@ PyObject* rmsnorm_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
     kt_ctx* ctx = address<kt_ctx>(a[0]);
     kt_status st;
     Py_BEGIN_ALLOW_THREADS
-    st = g_rmsnorm_quant(ctx, x, residual.ref, sum.ref, gain, eps, a[7] != Py_None ? &spec : nullptr, codes, scales,
-                         values.ref);
+    st = call(ctx, x, residual.ref, sum.ref, gain, eps, a[7] != Py_None ? &spec : nullptr, codes, scales, values.ref);
     Py_END_ALLOW_THREADS
     return st;
   });
@@ -141,6 +148,7 @@ PyObject* rmsnorm_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // ctx, device, cache, batch, q, k, v, rope, hadamard, asymmetric, clip, q_out, k_values, v_values -> status
 PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded<14>(n, [&] {
+    const auto call = bound(g_kv_append);
     const int dev = integer32(a[1], "device");
     const kt_kv_cache* cache = address<kt_kv_cache>(a[2]);
     const kt_kv_batch* batch = address<kt_kv_batch>(a[3]);
@@ -162,8 +170,7 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     kt_ctx* ctx = address<kt_ctx>(a[0]);
     kt_status st;
     Py_BEGIN_ALLOW_THREADS
-    st = g_kv_append(ctx, cache, batch, q.ref, k, v, rope, rope_rows, hadamard, &spec, q_out.ref, k_values.ref,
-                     v_values.ref);
+    st = call(ctx, cache, batch, q.ref, k, v, rope, rope_rows, hadamard, &spec, q_out.ref, k_values.ref, v_values.ref);
     Py_END_ALLOW_THREADS
     return st;
   });
@@ -172,6 +179,7 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // ctx, device, cache, batch, q, out, lse, scale, causal, window, scratch, scratch_bytes -> status
 PyObject* kv_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded<12>(n, [&] {
+    const auto call = bound(g_kv_attend);
     const int dev = integer32(a[1], "device");
     const kt_kv_cache* cache = address<kt_kv_cache>(a[2]);
     const kt_mat q = matrix(a[4], dev, "q"), out = matrix(a[5], dev, "out");
@@ -184,7 +192,7 @@ PyObject* kv_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     kt_ctx* ctx = address<kt_ctx>(a[0]);
     kt_status st;
     Py_BEGIN_ALLOW_THREADS
-    st = g_kv_attend(ctx, cache, batch, q, out, lse, scale, causal, window, scratch, bytes);
+    st = call(ctx, cache, batch, q, out, lse, scale, causal, window, scratch, bytes);
     Py_END_ALLOW_THREADS
     return st;
   });
@@ -204,4 +212,11 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_serving", "the serving calls of
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__serving() { return PyModule_Create(&g_module); }
+PyMODINIT_FUNC PyInit__serving() {
+  PyObject* m = PyModule_Create(&g_module);
+  if (m != nullptr && PyModule_AddStringConstant(m, "built_for", KT_BUILT_FOR) < 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}

@@ -89,6 +89,29 @@ REDUCE_FN = C.CFUNCTYPE(C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32,
 _lib = _serving = None
 
 
+class _Missing:
+    """Stands for _serving.so where it cannot be used: the serving calls raise the reason, all others need only the library."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError(self._why)
+
+
+def _load_serving():
+    """The module that reads the serving calls' tensors, built beside the library."""
+    from . import build
+    try:
+        from . import _serving as module
+    except ImportError as e:
+        return _Missing(f"the serving calls need _serving.so; build with: python -m paper_2503_01483_b200.build ({e})")
+    if module.built_for != build.built_for():
+        return _Missing(f"_serving.so was built for {module.built_for}, this is {build.built_for()}; build with: "
+                        "python -m paper_2503_01483_b200.build")
+    return module
+
+
 def lib():
     """Loads libkurtail.so (built by paper_2503_01483_b200.build).  Raises if absent."""
     global _lib, _serving
@@ -146,8 +169,9 @@ def lib():
         fn = getattr(L, name)
         if name not in ("kt_default_config", "kt_destroy", "kt_status_string"):
             fn.restype = i32
-    from . import _serving   # (built beside the library; a missing one raises as a missing library does)
-    _serving.bind(*(C.cast(getattr(L, n), vp).value for n in ("kt_rmsnorm_quant", "kt_kv_append", "kt_kv_attend")))
+    _serving = _load_serving()
+    if not isinstance(_serving, _Missing):
+        _serving.bind(*(C.cast(getattr(L, n), vp).value for n in ("kt_rmsnorm_quant", "kt_kv_append", "kt_kv_attend")))
     _lib = L
     return L
 

@@ -1,4 +1,8 @@
 """Host-side promises of the serving calls' Python side that need no GPU."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -61,3 +65,57 @@ def test_strides_of_single_columns_and_rows_say_nothing():
     for t in (x[:2].t(), x[:, ::2], x[:, :1].t()):
         with pytest.raises(ValueError):
             call(t)
+
+
+WITHOUT = """
+import sys, torch
+{before}
+from paper_2503_01483_b200 import kurtail
+assert kurtail.lib().kt_status_string(0) and kurtail.default_config().eps > 0     # the library's other calls work
+ctx = object.__new__(kurtail.Context)
+ctx._h, ctx._at, ctx._index, ctx.stream = None, 0, -1, None
+x = torch.zeros(1, 64)
+try:
+    ctx.rmsnorm_quant(x, bits=None, values=x)
+except ImportError as e:
+    assert {text!r} in str(e), e
+else:
+    raise SystemExit("no error")
+"""
+
+
+@pytest.mark.parametrize("before,text", [
+    ("sys.modules['paper_2503_01483_b200._serving'] = None", "_serving.so"),
+    ("import paper_2503_01483_b200.build as b; b.built_for = lambda: 'Python 2.7, torch 0.1'", "this is Python 2.7, torch 0.1")])
+def test_the_library_works_without_the_serving_module(before, text):
+    build.build()
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", WITHOUT.format(before=before, text=text)], cwd=root, capture_output=True,
+                       text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
+
+
+def test_a_serving_module_of_another_torch_is_built_anew(monkeypatch):
+    build.build()
+    assert not build.needs_build()
+    monkeypatch.setattr(build, "built_for", lambda: "Python 2.7, torch 0.1")
+    assert build.needs_build()
+
+
+def test_the_serving_module_needs_the_library_first():
+    # its entry points are null until lib() binds them
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = """
+import torch
+from paper_2503_01483_b200 import _serving
+x = torch.zeros(1, 64)
+try:
+    _serving.rmsnorm_quant(0, -1, x, None, None, None, 1e-6, None, 1.0, None, None, x)
+except ValueError as e:
+    assert "not loaded" in str(e), e
+else:
+    raise SystemExit("no error")
+"""
+    build.build()
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
