@@ -49,6 +49,22 @@ static kt_status opt_in(SmemOptIn* o, K kernel, int device, int bytes) {
   return KT_OK;
 }
 
+// CTAs of a kernel that an SM holds, `most` at most; asked for once per kernel and device.
+struct Residency {
+  int held[kMaxDevices];
+};
+template <typename K>
+static kt_status resident(Residency* r, K kernel, int device, int threads, int bytes, int most, int* per_sm) {
+  std::lock_guard<std::mutex> lock(g_optin_mutex);
+  *per_sm = device < kMaxDevices ? r->held[device] : 0;
+  if (*per_sm > 0) return KT_OK;
+  SV_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(per_sm, kernel, threads, bytes));
+  if (*per_sm < 1) return KT_ERR_CUDA;
+  if (*per_sm > most) *per_sm = most;
+  if (device < kMaxDevices) r->held[device] = *per_sm;
+  return KT_OK;
+}
+
 // ------------------------------------------------------------------------------------------------ RMSNorm
 static kt_status check_rows(const kt_mat& m, int64_t rows, int64_t cols) {
   if (m.data == nullptr && rows > 0) return KT_ERR_INVALID_ARG;
@@ -381,16 +397,11 @@ template <int HD, int BITS, int NT>
 static kt_status launch_rows(ServeCtx* sc, const AttendParams& p, const AttendPlan& pl) {
   using Cfg = AttendConfig<HD, BITS, NT, kRowWarps, kRowStages>;
   static SmemOptIn optin;
-  static int held[kMaxDevices];  // CTAs an SM holds
+  static Residency residency;
   auto kernel = k_kv_attend_rows<HD, BITS, NT, kRowWarps, kRowStages>;
   SV_TRY(opt_in(&optin, kernel, sc->device, Cfg::kSmem));
-  int per_sm = sc->device < kMaxDevices ? held[sc->device] : 0;
-  if (per_sm == 0) {
-    SV_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kRowWarps * 32, Cfg::kSmem));
-    if (per_sm < 1) return KT_ERR_CUDA;
-    if (per_sm > kRowCtas) per_sm = kRowCtas;
-    if (sc->device < kMaxDevices) held[sc->device] = per_sm;
-  }
+  int per_sm;
+  SV_TRY(resident(&residency, kernel, sc->device, kRowWarps * 32, Cfg::kSmem, kRowCtas, &per_sm));
   const int ctas = per_sm * sc->sm_count;
   SV_TRY(launch_early(sc, kernel, ctas, kRowWarps * 32, Cfg::kSmem, p));
   // A CTA a row while those are few: their blocks may have hundreds of parts each (8 query heads on one key head over 131072

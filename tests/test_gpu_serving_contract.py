@@ -1,6 +1,7 @@
 """What the header promises of the serving operators where single cases could miss it: NaN that a row sees, batches whose
 indices do not fit together, page tables that are columns of wider ones."""
-import numpy as np
+import threading
+
 import pytest
 import torch
 
@@ -45,14 +46,11 @@ def token_sets(n):
     return sets
 
 
-@pytest.mark.parametrize("layout", list(LAYOUTS))
-@pytest.mark.parametrize("tokens", ["newest", "last tiles", "first tiles", "inside"])
+@pytest.mark.parametrize("layout,tokens", [(x, t) for x in LAYOUTS for t in token_sets(LAYOUTS[x][1][0])])
 @pytest.mark.parametrize("name,kind", [("k", "scale"), ("k", "shift"), ("v", "scale"), ("v", "shift"), ("v", "inf")])
 @pytest.mark.parametrize("far", [False, True])
 def test_a_row_that_sees_what_is_no_number_gets_nan(ctx, layout, tokens, name, kind, far):  # noqa: F811
     n = LAYOUTS[layout][1][0]
-    if tokens not in token_sets(n):
-        pytest.skip("the sequence is too short")
     sq, cache, q, group, broken = poisoned(layout, name, token_sets(n)[tokens], far, kind)
     batch = sq.batch(ctx, cache, 2 * group)
     lse = torch.zeros(sq.N, 2 * group, device=DEV)
@@ -199,3 +197,46 @@ def test_a_row_is_one_whatever_its_stride(ctx):  # noqa: F811
         outs.append(ctx.kv_attend(cache, batch, ctx.kv_append(cache, batch, q, q[:, :hd], q[:, hd : 2 * hd])))
     ctx.check()
     assert torch.equal(*outs) and torch.equal(caches[0].k_codes, caches[1].k_codes)
+
+
+# ------------------------------------------------------------------------------------------------- threads
+def test_threads_with_a_context_each():
+    """Calls of several shapes from three threads at once, the first of a shape among them, against calls in a row."""
+    shapes = [(64, 4, [1, 1], 2), (64, 8, [3], 4), (128, 4, [2, 1], 8), (128, 8, [1], 3), (64, 4, [70], 2), (128, 8, [40, 1], 4)]
+    cases = []
+    for i, (hd, bits, rows, group) in enumerate(shapes):
+        sq = Seqs(rows, [r + 500 for r in rows], 32, seed=i)
+        cache, _, _ = filled_cache(sq, 2, hd, bits, seed=i, garbage=False)
+        x = rand(i, sq.N, 2 * (group + 1) * hd).to(BF16).to(DEV)
+        cases.append((sq, cache, x[:, : 2 * group * hd], x[:, 2 * group * hd :], 2 * group))
+    torch.cuda.synchronize()
+    results, errors = [None] * 4, []
+
+    def work(n):
+        try:
+            c = kurtail.Context(DEV, stream=torch.cuda.Stream(DEV))
+            got = []
+            with torch.cuda.stream(c.stream):
+                for sq, cache, q, k, heads in cases:
+                    own = kurtail.KvCache(*(t.clone() for t in (cache.k_codes, cache.v_codes, cache.k_steps, cache.v_steps)), cache.bits)
+                    batch = sq.batch(c, own, heads)
+                    _, s, v = c.rmsnorm_quant(q, bits=8, values=torch.empty(q.shape, dtype=BF16, device=DEV))
+                    qt = c.kv_append(own, batch, v, k, k, hadamard=True)
+                    got.append((s, qt, c.kv_attend(own, batch, qt), own.k_codes))
+                c.check()
+            results[n] = got
+            c.close()
+        except Exception as e:   # (a thread's own failure would be lost)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(n,)) for n in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    work(3)
+    assert not errors, errors
+    for n in range(3):
+        for a, b in zip(results[n], results[3]):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
