@@ -2,12 +2,13 @@
 indices do not fit together, page tables that are columns of wider ones."""
 import threading
 
+import numpy as np
 import pytest
 import torch
 
 from oracle import serving_oracle as so
 from paper_2503_01483_b200 import kurtail
-from test_gpu_serving import BF16, DEV, Seqs, ctx, filled_cache, rand  # noqa: F401
+from test_gpu_serving import BF16, DEV, Seqs, ctx, filled_cache, host, rand  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -240,3 +241,53 @@ def test_threads_with_a_context_each():
     for n in range(3):
         for a, b in zip(results[n], results[3]):
             assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+# ------------------------------------------------------------------------------------------------- roundings of few rows
+@pytest.mark.parametrize("rows,lengths,group", [([1] * 4, [1, 2, 3, 40], 4), ([3, 1, 2], [3, 70, 200], 4), ([1], [900], 8)])
+@pytest.mark.parametrize("hd,bits", [(128, 4), (128, 8), (64, 4), (64, 8)])
+def test_few_rows_round_products_to_float16_and_no_further(ctx, rows, lengths, group, hd, bits):  # noqa: F811
+    """Values whose codes lie at one end of their range and whose shifts bring them near zero: the result is small beside the
+    products p s u that it is summed from, so their rounding shows (with bf16 it is 8 times the bound).
+
+    Keys are flat (scale 0), so a score is shift times sum(q), in float32: the sum of hd terms, at most hd / 4 + 2 of them one
+    after another in a lane and across lanes, and four products, 2^-24 each; the exponential 2^-22 of itself.  With |score| <= S
+    a probability is off by the factor exp(2 (hd / 4 + 6) 2^-24 S) and 2^-21.  p s: half a step of float16, 2^-11 of itself, and
+    of float16's smallest step, 2^-25 against a largest of at least 2^2 (2^-27 of it; 2^-26 leaves room for a reference that
+    moved).  Sums in float32: 2^-24 for each of the sequence's tokens and runs.  The result: half a step of bf16, 2^-8.  In norm
+    that last error is uniform: 2^-8 / sqrt(3)."""
+    mid = 2 ** (bits - 1)
+    sq = Seqs(rows, lengths, 16, seed=bits)
+    g = np.random.RandomState(hd + bits)
+    shape = (sq.pages, 2, 16)
+    u = {n: g.randint(2 * mid - mid // 4, 2 * mid, (*shape, hd)).astype(np.uint8) for n in "kv"}
+    k_steps = np.stack((np.zeros(shape), g.uniform(-1.0, 1.0, shape)), -1).astype(np.float32)
+    scale_v = g.uniform(0.5, 1.5, shape)
+    v_steps = np.stack((scale_v, -scale_v * (2 * mid - mid / 8)), -1).astype(np.float32)
+    dev = lambda a: torch.tensor(a, device=DEV)  # noqa: E731
+    cache = kurtail.KvCache(dev(so.pack(u["k"], bits)), dev(so.pack(u["v"], bits)), dev(k_steps), dev(v_steps), bits)
+    q = rand(bits, sq.N, 2 * group * hd).abs().to(BF16).to(DEV)
+    out = ctx.kv_attend(cache, sq.batch(ctx, cache, 2 * group), q, scale=1.0 / hd)
+    ctx.check()
+    got, err, ref, rest = host(out).astype(np.float64), [], [], []
+    for s, (r, n) in enumerate(zip(rows, lengths)):
+        at = np.array([sq.at(s, j) for j in range(n)])
+        at = (at[:, 0], at[:, 1])
+        see = so.visible(r, n)
+        for head in range(2 * group):
+            kh = head // group
+            cols, own = slice(head * hd, (head + 1) * hd), slice(sq.starts[s], sq.starts[s + 1])
+            part = [a[at[0], kh, at[1]] for a in (u["k"], k_steps, u["v"], v_steps)]
+            qq = host(q[own, cols])
+            o, _, spread, size = so.attend(qq, *part, see, 1.0 / hd)
+            S = np.abs(qq).astype(np.float64).sum(1).max() / hd
+            moves = np.expm1(2 * (hd / 4 + 6) * 2.0**-24 * S) + 2.0**-21 + n * 2.0**-24
+            # (a term p v enters as p s (u - middle) and p times the middle's value)
+            parts = spread + np.abs(part[3][:, 0] * mid + part[3][:, 1]).max()
+            low = 2.0**-26 * part[3][:, 0].max() * mid * n
+            tol = (2.0**-11 * 1.001) * spread + 2 * moves * parts + low
+            diff = np.abs(got[own, cols] - o)
+            assert (diff <= 2.0**-8 * (np.abs(o) + tol) + tol).all(), np.max(diff / (2.0**-8 * np.abs(o) + tol))
+            err.append(diff.ravel()), ref.append(o.ravel()), rest.append(tol.ravel())
+    norm = lambda x: np.linalg.norm(np.concatenate(x))  # noqa: E731
+    assert norm(err) <= 1.05 * 2.0**-8 / np.sqrt(3.0) * norm(ref) + norm(rest)
