@@ -8,7 +8,7 @@ import torch
 
 from oracle import serving_oracle as so
 from paper_2503_01483_b200 import kurtail
-from test_gpu_serving import BF16, DEV, Seqs, ctx, filled_cache, host, rand  # noqa: F401
+from test_gpu_serving import BF16, DEV, Seqs, close_attention, ctx, filled_cache, host, rand, rope_table  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -198,6 +198,69 @@ def test_a_row_is_one_whatever_its_stride(ctx):  # noqa: F811
         outs.append(ctx.kv_attend(cache, batch, ctx.kv_append(cache, batch, q, q[:, :hd], q[:, hd : 2 * hd])))
     ctx.check()
     assert torch.equal(*outs) and torch.equal(caches[0].k_codes, caches[1].k_codes)
+
+
+# ------------------------------------------------------------------------------------------------- many sequences, many heads
+@pytest.mark.parametrize("hd,bits,most_rows", [(64, 4, 2), (128, 8, 3), (64, 8, 40)])
+def test_thousands_of_sequences(ctx, hd, bits, most_rows):  # noqa: F811
+    # more than the attention's list keeps sums of, and three levels of the append's search
+    g = np.random.RandomState(hd)
+    n, heads, group = 4100, 1, 4
+    rows = g.randint(0, most_rows + 1, n) * (g.rand(n) < 0.7)
+    lengths = rows + np.where(g.rand(n) < 0.5, 0, g.randint(0, 60, n))
+    lengths[g.rand(n) < 0.002] += 400
+    sq = Seqs(rows, lengths, 16, seed=1, pad=5)
+    cache, codes, steps = filled_cache(sq, heads, hd, bits, seed=2)
+    q = rand(1, sq.N, heads * group * hd).to(BF16).to(DEV)
+    batch = sq.batch(ctx, cache, heads * group)
+    some = [s for s in [0, 1, 31, 32, 1023, 1024, 1025, n - 1, *np.argsort(-lengths)[:4], *g.randint(0, n, 60)]]
+    close_attention(ctx, cache, codes, steps, sq, q, batch, hd, heads, group, hd**-0.5, True, 0, sequences=some)
+    # each row of the append lands where a call for its sequence alone puts it
+    k = rand(3, sq.N, hd).to(BF16).to(DEV)
+    rope = rope_table(int(lengths.max()), hd)
+    into = kurtail.KvCache.empty(sq.pages, 1, 16, hd, bits, DEV)
+    ctx.kv_append(into, batch, None, k, k, rope=rope, hadamard=True)
+    ctx.check()
+    i32 = lambda a: torch.tensor(np.asarray(a, np.int32), device=DEV)  # noqa: E731
+    alone = kurtail.KvCache.empty(sq.pages, 1, 16, hd, bits, DEV)
+    for s in some:
+        r = int(rows[s])
+        one = ctx.kv_batch(alone, 1, i32([0, r]), i32([lengths[s]]), i32(sq.table[s : s + 1]), max(r, 1), max(int(lengths[s]), 1))
+        part = k[int(sq.starts[s]) : int(sq.starts[s]) + r]
+        ctx.kv_append(alone, one, None, part, part, rope=rope, hadamard=True)
+        used = [p for p in sq.table[s, : -(-int(lengths[s]) // 16)]]
+        for a, b in ((into.k_codes, alone.k_codes), (into.v_steps, alone.v_steps)):
+            assert torch.equal(a[used], b[used]), s
+    assert int((into.k_steps[..., 0] > 0).sum()) == int(rows.sum())
+    ctx.check()
+
+
+@pytest.mark.parametrize("group", [100, 128, 129, 200, 300])
+def test_many_query_heads_on_one_key_head(ctx, group):  # noqa: F811
+    sq = Seqs([1, 0, 1], [300, 10, 40], 32, pad=1)
+    cache, codes, steps = filled_cache(sq, 1, 64, 4, seed=2)
+    q = rand(1, sq.N, group * 64).to(BF16).to(DEV)
+    close_attention(ctx, cache, codes, steps, sq, q, sq.batch(ctx, cache, group), 64, 1, group, 0.125, True, 0)
+
+
+@pytest.mark.parametrize("rows,group", [([2, 3], 4), ([70, 9], 4)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_a_query_that_is_no_number_touches_its_own_row_only(ctx, rows, group, value):  # noqa: F811
+    hd = 64
+    sq = Seqs(rows, [r + 200 for r in rows], 32)
+    cache, _, _ = filled_cache(sq, 2, hd, 8, seed=2)
+    q = rand(1, sq.N, 2 * group * hd).to(BF16).to(DEV)
+    batch = sq.batch(ctx, cache, 2 * group)
+    lse = [torch.zeros(sq.N, 2 * group, device=DEV) for _ in range(2)]
+    want = ctx.kv_attend(cache, batch, q, lse=lse[0]).clone()
+    q[1, 3 * hd + 7] = value
+    got = ctx.kv_attend(cache, batch, q, lse=lse[1])
+    ctx.check()
+    hit = torch.zeros(sq.N, 2 * group, dtype=torch.bool, device=DEV)
+    hit[1, 3] = True
+    got, want = got.view(sq.N, 2 * group, hd), want.view(sq.N, 2 * group, hd)
+    assert torch.equal(got[~hit], want[~hit]) and torch.equal(lse[0][~hit], lse[1][~hit])
+    assert bool(got[hit].isnan().all()) and bool(lse[1][hit].isnan().all())
 
 
 # ------------------------------------------------------------------------------------------------- threads
