@@ -476,7 +476,7 @@ kt_status kt_quant4_codes(kt_ctx* ctx, const float* Y, int64_t N, int64_t d, int
  * y and `codes` and `scales` must be NULL.
  * X, residual, sum: N x d, one type (KT_BF16 or KT_F32), any N >= 0, d in
  * 1..32768, any alignment of the element (16-byte aligned rows with d a multiple
- * of 8 are fastest); `sum` (may be NULL; needs a residual) receives h and may
+ * of 8 are fastest; of others the aligned 16 bytes around a row's ends are read); `sum` (may be NULL; needs a residual) receives h and may
  * be X's or residual's own matrix.  gain: d float32 or NULL.  codes (N x d int8,
  * dense) and values (KT_BF16 or KT_F32) may each be NULL, not both; scales: N
  * float32.  A row that holds a NaN or an infinity (or overflows float32) gets
@@ -553,15 +553,24 @@ kt_status kt_kv_append(kt_ctx* ctx, const kt_kv_cache* cache, const kt_kv_batch*
  *   out = sum_j softmax_j(scale q.k_j) v_j (KT_BF16),
  *   lse = log sum_j exp(scale q.k_j) (float32, dense rows x q_heads; NULL: not wanted).
  * scale in 0..1e30 (KT_ERR_INVALID_ARG otherwise).
+ * Roundings: scores, softmax statistics and sums are float32.  Up to 128 rows of a
+ * key head (max_rows q_heads / heads): the probability times the value's scale is
+ * rounded to float16 (2^-11 of itself), codes and shifts enter exactly.  More rows:
+ * probabilities are rounded to bf16, and so are the values that codes stand for
+ * (2^-8 of themselves each; 8-bit codes lose their last bits, and more where a
+ * head's shift is large beside its range).  Probabilities are summed against a
+ * reference up to 2^8 below the maximum: values of a size that times the
+ * sequence's tokens stays below 1e36 keep the sums finite.
  * A row that sees no token gets zeros and lse -inf.  Tokens that a row does not
  * see never touch it, whatever they hold; a row that sees a token whose scale or
  * shift is NaN, or whose value's is an infinity, gets NaN, out and lse.  out may be
- * Q's own matrix.  `scratch` (device, 256-byte aligned, not the context's workspace) holds kt_kv_scratch_bytes() bytes for this cache, batch
- * and head count; its contents matter only during the call, and two calls that
- * may overlap need two.  A sequence whose rows or length are out of their bounds
- * is skipped, its rows left as they were; rows of a sequence with a page id out
- * of range are written, with unspecified values.  Matrices need 16-byte aligned
- * bases and leading dimensions. */
+ * Q's own matrix.  `scratch` (device, 256-byte aligned, not the context's
+ * workspace) holds kt_kv_scratch_bytes() bytes for this cache, batch and head
+ * count; its contents matter only during the call, and two calls that may overlap
+ * need two.  A sequence whose rows or length are out of their bounds is skipped,
+ * its rows left as they were; rows of a sequence with a page id out of range are
+ * written, with unspecified values.  Matrices need 16-byte aligned bases and
+ * leading dimensions. */
 kt_status kt_kv_scratch_bytes(const kt_ctx* ctx, const kt_kv_cache* cache, const kt_kv_batch* batch,
                               int32_t q_heads, size_t* bytes);
 kt_status kt_kv_attend(kt_ctx* ctx, const kt_kv_cache* cache, const kt_kv_batch* batch, kt_mat Q, kt_mat out,

@@ -301,9 +301,11 @@ constexpr int kRowWarps = 4, kRowStages = 3;
 constexpr int kRowCtas = 4;  // CTAs an SM is given runs for, where it holds as many
 
 // Rows of a key head from which the tensor-memory kernel is used.  Its tile is 256 rows, it reads what a first kernel has
-// unpacked, and its smallest run is four tiles of tokens: up to 128 rows the rows kernel is faster, though it reads the
-// cache once per 16 rows (one sequence of 32768 tokens, 8 key heads: 16 tokens by 4 heads 60 against 102 us; four of
-// 8192, 32 tokens by 4 heads 104 against 110 us; one of 500 19 against 22 us).
+// unpacked, and its smallest run is two tiles of tokens; the rows kernel reads and converts the cache once per 16 rows.  At
+// 128 rows the two meet (rows against tiles, 8 key heads of 128, 4 bits: one sequence of 32768 tokens 97 and 98 us, of 8192
+// 37 and 41, of 500 18 and 21, four of 8192 101 and 94), the rows kernel behind where there are many tokens (16 sequences of
+// 2000 115 and 89, one of 131072 in 8 bits 524 and 339); at 64 it is far ahead (32768 tokens 54 and 97 us), at 256 behind
+// (184 and 103).
 constexpr long long kPromptRows = 129;
 // Unpacked tiles held at a time; longer batches go in groups of sequences (one at least).
 constexpr size_t kTileBudget = 1ull << 30;

@@ -6,12 +6,15 @@
 //   sum_t p_t v_t  = sum_t (p_t s_t) u_t + sum_t p_t b_t
 // and the codes themselves (centred on zero) are the operands of the tensor cores: small integers are exact in float16,
 // so no rounding of the cache is added, and no entry is ever scaled.  float16 and not bf16, because its ten fraction bits
-// take a 4-bit code from either half of a byte, or an 8-bit code, without a shift: what bounds this kernel is the logic
-// that turns codes into operands (ALU pipe 72 % busy with bf16 at 64 sequences of 8192 tokens, 4 bits).  The other
-// operands get a power of two that keeps them inside float16's range: a query row the one that brings its largest entry
-// to 2^14 (exact; entries below 2^-28 of the largest lose bits), p_t s_t the one that brings the row's largest p_t s_t so
-// far to 2^2 (terms below 2^-16 of it lose bits: 2^-28 of it each at most).  Rounding p_t s_t to float16 (2^-11 of itself at most)
-// is the only rounding before the output's; scores, softmax statistics, sums and outputs are float32.
+// take a 4-bit code from either half of a byte, or an 8-bit code, without a shift: turning codes into operands is most of
+// this kernel's instructions (64 sequences of up to 8192 tokens, 4 bits: with bf16 the ALU pipe was 72 % busy, with float16
+// it is 48 %, issue slots 60 %; no unit is full, and 16 warps an SM do not hide each other's latencies).  The other
+// operands get a power of two that keeps them inside float16's range.  A query row: the one that brings its largest entry to
+// 2^14.  Its bf16 entries are exact then down to 2^-31 of that power of two; with 4-bit codes the odd ones, which are held 16
+// times smaller, down to 2^-27; smaller ones are off by 2^-39 (odd ones 2^-35) of it at most.  p_t s_t: the one that brings the
+// row's largest p_t s_t so far to 2^2 (terms below 2^-16 of it are off by 2^-27 of it at most).  Rounding p_t s_t to float16,
+// 2^-11 of itself at most, is the only other rounding before the output's; scores, softmax statistics, sums and outputs are
+// float32.
 //
 // Layout of the work.  A row is a query head of one token; the rows of one key head (group x tokens) are packed into
 // blocks of 8 NT.  All tiles of 32 tokens of all blocks form one list, cut into equal runs, one per CTA that the device

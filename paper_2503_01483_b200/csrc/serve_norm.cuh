@@ -7,7 +7,7 @@
 //
 // One pass over the data: a row stays in registers between the sum of squares and the codes.  What bounds it is HBM
 // (7 bytes an entry with a bf16 residual and codes); a row of up to 1024 entries belongs to one warp or a part of
-// it (no block barrier), a wider one to a block of up to 1024 threads that hold 8 to 32 entries each.
+// it (no block barrier), a wider one to a block of up to 1024 threads that hold 16 or 32 entries each.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -137,7 +137,7 @@ __device__ __forceinline__ void stored2(float& a, float& b, const __nv_bfloat16*
 
 // Eight entries of a row from j0 on, whatever their alignment, entries outside 0 .. d - 1 as zeros: the aligned 16-byte
 // pieces that hold them (a piece that holds none of the row is not read), shifted into place.  The shift is the same for
-// all groups of a row.
+// all groups of a row.  (A row's first and last piece may hold up to 14 bytes of what lies beside it: read, never used.)
 template <typename T>
 __device__ __forceinline__ void load8_any(const T* row, int j0, int d, float (&v)[8]) {
   constexpr int N = sizeof(T) / 2 + 1;  // pieces
