@@ -106,8 +106,9 @@ def _load_serving():
         from . import _serving as module
     except ImportError as e:
         return _Missing(f"the serving calls need _serving.so; build with: python -m paper_2503_01483_b200.build ({e})")
-    if module.built_for != build.built_for():
-        return _Missing(f"_serving.so was built for {module.built_for}, this is {build.built_for()}; build with: "
+    named = getattr(module, "built_for", "another version of this library")
+    if named != build.built_for():
+        return _Missing(f"_serving.so was built for {named}, this is {build.built_for()}; build with: "
                         "python -m paper_2503_01483_b200.build")
     return module
 

@@ -86,6 +86,7 @@ else:
 
 @pytest.mark.parametrize("before,text", [
     ("sys.modules['paper_2503_01483_b200._serving'] = None", "_serving.so"),
+    ("import paper_2503_01483_b200._serving as m; del m.built_for", "another version of this library"),
     ("import paper_2503_01483_b200.build as b; b.built_for = lambda: 'Python 2.7, torch 0.1'", "this is Python 2.7, torch 0.1")])
 def test_the_library_works_without_the_serving_module(before, text):
     build.build()
