@@ -476,12 +476,12 @@ kt_status kt_quant4_codes(kt_ctx* ctx, const float* Y, int64_t N, int64_t d, int
  * y and `codes` and `scales` must be NULL.
  * X, residual, sum: N x d, one type (KT_BF16 or KT_F32), any N >= 0, d in
  * 1..32768, any alignment of the element (16-byte aligned rows with d a multiple
- * of 8 are fastest; of others the aligned 16 bytes around a row's ends are read); `sum` (may be NULL; needs a residual) receives h and may
- * be X's or residual's own matrix.  gain: d float32 or NULL.  codes (N x d int8,
- * dense) and values (KT_BF16 or KT_F32) may each be NULL, not both; scales: N
- * float32.  A row that holds a NaN or an infinity (or overflows float32) gets
- * scale NaN, codes 0 and values NaN.  KT_ERR_INVALID_ARG for spec->asymmetric
- * and clip_mode 1. */
+ * of 8 are fastest; of others the aligned 16 bytes around a row's ends are read);
+ * `sum` (may be NULL; needs a residual) receives h and may be X's or residual's own
+ * matrix.  gain: d float32 or NULL.  codes (N x d int8, dense) and values (KT_BF16
+ * or KT_F32) may each be NULL, not both; scales: N float32.  A row that holds a NaN
+ * or an infinity (or overflows float32) gets scale NaN, codes 0 and values NaN.
+ * KT_ERR_INVALID_ARG for spec->asymmetric and clip_mode 1. */
 kt_status kt_rmsnorm_quant(kt_ctx* ctx, kt_mat X, const kt_mat* residual, const kt_mat* sum, const float* gain,
                            double eps, const kt_quant_spec* spec, int8_t* codes, float* scales,
                            const kt_mat* values);
@@ -518,7 +518,8 @@ typedef struct {
   int32_t n_seqs;
   int32_t table_ld;          /* columns: page ids are followed up to this one */
   int32_t max_rows;          /* no sequence has more rows (2^30 at most; attention: times the
-                                query heads of a key head, 2^31 - 256 at most) */
+                                query heads of a key head, 2^31 - 256 at most, and above
+                                128 all sequences go through the prompts' kernel) */
   int32_t max_length;        /* no sequence has more tokens (2^30 at most) */
 } kt_kv_batch;
 

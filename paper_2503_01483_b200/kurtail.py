@@ -263,7 +263,9 @@ class KvBatch:
     """The sequences of a call (kt_kv_batch) and the scratch of their attention; made by Context.kv_batch().
 
     The three index tensors may be rewritten in place between calls and between replays of a captured graph, within
-    max_rows and max_length (lowered to what page_table's own columns hold, where it is columns of a wider table).  Two calls that may overlap need two KvBatch objects (each owns one scratch buffer).
+    max_rows and max_length (lowered to what page_table's own columns hold, where it is columns of a wider table).  max_rows
+    chooses the attention's kernel for all sequences of a call: single tokens beside a prompt are served faster by a call of
+    their own.  Two calls that may overlap need two KvBatch objects (each owns one scratch buffer).
     """
 
     def __init__(self, row_starts, lengths, page_table, max_rows, max_length):
