@@ -622,7 +622,8 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 2) k_kv_attend_rows(
               if (none) pr = 0.f;
               l[nt][i] += pr;
               bs[nt][i] += none ? 0.f : pr * fb;  // (not 0 times what a hidden token may hold)
-              w[i] = none ? 0.f : pr * (vf[mt][half].x * held_up(big[nt][i]));
+              // (p first: s times the power of two may pass float32's range where p is 0)
+              w[i] = none ? 0.f : pr * vf[mt][half].x * held_up(big[nt][i]);
             }
             pf[nt][mt][half] = transpose8x8(pack_f16(w[0], w[1]));
           }

@@ -66,6 +66,27 @@ def test_a_row_that_sees_what_is_no_number_gets_nan(ctx, layout, tokens, name, k
         assert bool(out[r, group:].isfinite().all()) and bool(lse[r, group:].isfinite().all())   # the other key head
 
 
+@pytest.mark.parametrize("layout", ["few", "few16", "many", "chunks"])
+def test_a_large_step_of_no_weight_beside_flat_values(ctx, layout):  # noqa: F811
+    # all values are one number each (scale 0), but for a token of a large scale whose probability is 0 in float32
+    sq, cache, q, group, _ = poisoned(layout, "v", [200], True, "shift")
+    p, o = sq.at(0, 200)
+    cache.v_steps[..., 0] = 0.0
+    cache.v_steps[..., 1] = rand(5, *cache.v_steps.shape[:3]).to(DEV)
+    batch = sq.batch(ctx, cache, 2 * group)
+    want = ctx.kv_attend(cache, batch, q).clone()
+    mid = 2.0 ** (cache.bits - 1)
+    for big in (2.0**26, 2.0**40, 2.0**90):
+        cache.v_steps[p, 0, o] = torch.tensor([big, -mid * big], device=DEV)
+        got = ctx.kv_attend(cache, batch, q)
+        ctx.check()
+        sees = so.visible(sq.rows[0], sq.lengths[0])
+        for r in range(sq.rows[0]):   # (the token's own row, in a prompt, gives it some weight)
+            if sees[r].sum() > 300:
+                assert torch.equal(got[r], want[r]), (big, r)
+        assert torch.equal(got[sq.rows[0] :][: -sq.pad], want[sq.rows[0] :][: -sq.pad])
+
+
 # ------------------------------------------------------------------------------------------------- host bounds
 @pytest.mark.parametrize("max_rows,group,fits", [(2**28, 16, False), (2**30, 2, False), (2**30, 64, False), (2**27, 16, False),
                                                  (2**30, 1, True), (2**27, 15, True)])
