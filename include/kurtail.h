@@ -560,8 +560,9 @@ kt_status kt_kv_append(kt_ctx* ctx, const kt_kv_cache* cache, const kt_kv_batch*
  * probabilities are rounded to bf16, and so are the values that codes stand for
  * (2^-8 of themselves each; 8-bit codes lose their last bits, and more where a
  * head's shift is large beside its range).  Probabilities are summed against a
- * reference up to 2^8 below the maximum: values of a size that times the
- * sequence's tokens stays below 1e36 keep the sums finite.
+ * reference up to 2^8 below the maximum: queries and keys within 1e30, and values
+ * of a size that times the sequence's tokens stays below 1e36, keep every sum
+ * finite.
  * A row that sees no token gets zeros and lse -inf.  Tokens that a row does not
  * see never touch it, whatever they hold; a row that sees a token whose scale or
  * shift is NaN, or whose value's is an infinity, gets NaN, out and lse.  out may be
