@@ -536,8 +536,8 @@ typedef struct {
  * (spec->bits == cache->bits, clip_mode 0) and stored; Q goes to Q_out (KT_BF16;
  * may be Q's own matrix).  K_values, V_values (KT_BF16, NULL: not wanted) receive
  * what the cache now stands for: the simulated quantisation of the paper's own
- * evaluation.  A head that holds a NaN or an infinity gets scale and shift NaN
- * and codes 0.  A row whose position, length or page is out of bounds is skipped,
+ * evaluation.  A head that holds a NaN or an infinity (or whose range or shift
+ * passes float32) gets scale and shift NaN and codes 0.  A row whose position, length or page is out of bounds is skipped,
  * and so are all rows of a sequence whose starts do not fit the matrices or
  * max_rows.  A sequence shorter than its rows is such an error here (its first rows
  * have no position), while kt_kv_attend takes these as rows that see nothing.

@@ -239,8 +239,8 @@ __device__ __forceinline__ void hold_head(const AppendParams& p, float (&y)[2][8
     scale = __fdiv_rn(__fmul_rn(max_nan(mx, -mn), p.clip), p.den);
     shift = __fmul_rn(-scale, kHalf);
   }
-  // an infinity or a NaN (or a range past float32): scale and shift NaN, codes 0
-  if (!(scale < __uint_as_float(0x7f800000u)) || !(fabsf(low) < __uint_as_float(0x7f800000u)))
+  // an infinity or a NaN (or a range, or a shift, past float32): scale and shift NaN, codes 0
+  if (!(scale < __uint_as_float(0x7f800000u)) || !(fabsf(shift) < __uint_as_float(0x7f800000u)))
     scale = shift = __uint_as_float(0x7fc00000u);
   const bool divide = quant_needs_division(scale), clamp = p.clip != 1.f;
   const float inv = divide ? 0.f : __frcp_rn(scale);

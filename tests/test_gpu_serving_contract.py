@@ -375,3 +375,27 @@ def test_few_rows_round_products_to_float16_and_no_further(ctx, rows, lengths, g
             err.append(diff.ravel()), ref.append(o.ravel()), rest.append(tol.ravel())
     norm = lambda x: np.linalg.norm(np.concatenate(x))  # noqa: E731
     assert norm(err) <= 1.05 * 2.0**-8 / np.sqrt(3.0) * norm(ref) + norm(rest)
+
+
+# ------------------------------------------------------------------------------------------------- the ends of float32
+@pytest.mark.parametrize("asym", [True, False])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_heads_whose_steps_pass_float32_are_no_numbers(ctx, asym, bits):  # noqa: F811
+    # symmetric: the shift is -2^(bits - 1) times the scale, past float32 for a head that is within it
+    hd = 64
+    x = torch.zeros(4, hd, device=DEV)
+    x[0], x[1, 3], x[2, 3], x[3, 5], x[3, 6] = 1.0, 3.4e38, 2.5e38, 3e38, -3e38
+    cache = kurtail.KvCache.empty(1, 1, 16, hd, bits, DEV)
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device=DEV)  # noqa: E731
+    batch = ctx.kv_batch(cache, 1, i32(0, 4), i32(4), i32(0)[None], 4, 4)
+    values = torch.zeros(4, hd, dtype=BF16, device=DEV)
+    ctx.kv_append(cache, batch, None, x, x, asymmetric=asym, v_values=values)
+    ctx.check()
+    with np.errstate(all="ignore"):
+        _, s, b, _ = so.held(x.cpu().numpy()[:, None], bits, asym, np.float32(1.0))
+    good = np.isfinite(s[:, 0]) & np.isfinite(b[:, 0])
+    assert good[0] and good[2] and not good[3 if asym else 1]
+    got = cache.v_steps[0, 0, :4].cpu().numpy()
+    assert np.array_equal(got[good, 0], s[good, 0]) and np.array_equal(got[good, 1], b[good, 0])
+    assert np.isnan(got[~good]).all() and bool(values[torch.tensor(~good)].isnan().all())
+    assert int(cache.v_codes[0, 0, :4][torch.tensor(~good)].max()) == 0
